@@ -1099,11 +1099,14 @@ def tern_mx_linear_grad(dy: torch.Tensor, w: Optional[MxTensor], saved: Optional
     dw = dy^T saved and db = the sums of dy's columns (bias=True) in float32.  w None: no dx; saved None: no dw."""
     good = all(q is None or q.__class__ is MxTensor for q in (w, saved)) and not (w is None and saved is None and not bias)
     if good and (w is None or w.kind == "f4" and len(w.shape) == 2) and (saved is None or saved.kind == "i8"):
-        done = _plain("mx_linear_grad", "tern_mx_linear_grad", dy, None if w is None else w.data,
-                      None if saved is None else saved.data, w.cols if w is not None else saved.cols if saved is not None else 1,
-                      bool(bias), workspace)
-        if done is not None:
-            return done
+        # (the compiled path sees bytes and c_in: other extents may fill up to as many bytes)
+        c_in = w.cols if w is not None else saved.cols if saved is not None else 1
+        if dy.__class__ is torch.Tensor and dy.dim() > 0 and (w is None or w.shape[0] == dy.shape[-1]) and (
+                saved is None or saved.shape == (*dy.shape[:-1], c_in)):
+            done = _plain("mx_linear_grad", "tern_mx_linear_grad", dy, None if w is None else w.data,
+                          None if saved is None else saved.data, c_in, bool(bias), workspace)
+            if done is not None:
+                return done
     t, rows, c_out, ldy = _matrix(dy, "dy")
     if w is None and saved is None and not bias:
         raise ValueError("nothing is asked for: w, saved and bias")
