@@ -106,21 +106,29 @@ __global__ __launch_bounds__(kThreads) void values_i8_kernel(const uint8_t* code
     if (left > 0) store_eight(out + row * ld + at, v, left < 8 ? (int)left : 8);
 }
 
-// e = exp(-|g|), as e.most e.rest, and r = 1 / (1 + e): the sigmoid of g is r for g >= 0 and e r below, and one less it the
-// other.  exp2 and reciprocal as the device has them (right to some 1e-7); exp2's result has no numbers below 2^-126,
-// so a factor of 2^-64 waits in e.rest where it would need them.
+// e = exp(-|g|) as 2^n m, n <= 0 and m in (1/2, 1], and r = 1 / (1 + e): the sigmoid of g is r for g >= 0 and e r below, and one less
+// it the other.  n is taken off -|g| log2(e) by fused operations with both halves of the constant, so that what exp2 gets is right
+// to 2^-24 whatever |g| is (rounded as a product it was |g| 2^-23 off: 1.0e-6 of e at |g| = 20, 3.8e-6 at 80); exp2 and the
+// reciprocal as the device has them (right to their last bit).  e itself may have no leading bit or be zero: n and m hold it.
 struct Decay {
-    float most, rest, r;
+    float m, r;
+    int n;
 };
 __device__ __forceinline__ Decay decay(float g)
 {
     Decay d;
-    const float x = fabsf(g) * -1.442695041f;
-    const bool deep = x < -120.0f;
-    d.most = __builtin_amdgcn_exp2f(deep ? x + 64.0f : x);
-    d.rest = deep ? 0x1p-64f : 1.0f;
-    d.r = __builtin_amdgcn_rcpf(1.0f + d.most * d.rest);
+    const float a = fabsf(g), n = fmaxf(__builtin_ceilf(a * -1.442695021629333f), -400.0f);     // (beyond: every product is zero)
+    d.n = (int)n;
+    d.m = __builtin_amdgcn_exp2f(__builtin_fmaf(a, -1.925963033500e-8f, __builtin_fmaf(a, -1.442695021629333f, -n)));
+    d.r = __builtin_amdgcn_rcpf(1.0f + __builtin_ldexpf(d.m, d.n));
     return d;
+}
+// v e p, |v p| less than 2^9 |v| or a result that overflows too: part of 2^n before the product, which keeps it within a float's range,
+// and the rest behind it.
+__device__ __forceinline__ float decayed(const Decay& d, float v, float p)
+{
+    const int first = max(d.n, -32);
+    return __builtin_ldexpf(p * (__builtin_ldexpf(v, first) * d.m), d.n - first);
 }
 
 template <typename T, bool SAVE>
@@ -138,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const T* gu, int64_t row
     for (int i = 0; i < 8; ++i) {
         const Decay d = decay(g[i]);
         const float a = g[i] * d.r;
-        y[i] = g[i] < 0.0f ? (a * (u[i] * d.most)) * d.rest : a * u[i];
+        y[i] = g[i] < 0.0f ? decayed(d, u[i], a) : a * u[i];
     }
     store_eight(h + row * ldh + at, y, n);
     if constexpr (SAVE) {
@@ -170,7 +178,7 @@ __global__ __launch_bounds__(kThreads) void gate_grad_kernel(const T* dh, int64_
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const Decay k = decay(g[i]);
-        const float small = k.most * k.rest * k.r, s = g[i] < 0.0f ? small : k.r, less = g[i] < 0.0f ? k.r : small, a = g[i] * s;
+        const float small = __builtin_ldexpf(k.m, k.n) * k.r, s = g[i] < 0.0f ? small : k.r, less = g[i] < 0.0f ? k.r : small, a = g[i] * s;
         y[i] = a * u[i];
         g[i] = d[i] * u[i] * (s + a * less);
         u[i] = d[i] * a;

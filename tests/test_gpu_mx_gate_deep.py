@@ -1,0 +1,63 @@
+"""The gate where exp(-|g|) is far below one, in float and bf16, against the 64-bit oracle: as near there as
+at zero.
+
+Bounds in units of 2^-23.  e = exp(-|g|) is 2^n exp2(f), f in (-1, 0] of two fused operations (0.35), exp2 right to its last
+bit (1); 1 / (1 + e): 0.7 of e, 0.5 of the sum, 1 of the reciprocal, 2.2.  h: e, the reciprocal and three products, 5.05,
+taken as 6."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1801_09449_amd as T
+from oracle import mx_oracle as O
+from tests.test_gpu_mx import HALF_ULP, f64
+
+pytestmark = pytest.mark.gpu
+UNIT = 2.0 ** -23
+# a result without a leading bit is stored to the nearest of those, and the product before it may be one too
+LEAST = {torch.float32: 2.0 ** -148, torch.bfloat16: 2.0 ** -133}
+
+
+def spread(seed, lo, hi, n=4096):
+    return lo + (hi - lo) * torch.rand(4, n, generator=torch.Generator().manual_seed(seed), dtype=torch.float64)
+
+
+def powers(seed, exponent):
+    """+-m 2^exponent, 1 <= m < 2, within float's range."""
+    r = torch.Generator().manual_seed(seed)
+    m = 1 + torch.rand(exponent.shape, generator=r, dtype=torch.float64)
+    sign = torch.randint(0, 2, exponent.shape, generator=r) * 2 - 1
+    return sign * m * torch.exp2(exponent.floor().clamp(-126, 126))
+
+
+@pytest.mark.parametrize("lo,hi", [(-4, 4), (-40, -4), (4, 80), (-87, -40)])
+def test_a_gate_in_float_is_as_near_at_every_size(lo, hi):
+    g, u = spread(1, lo, hi).float(), powers(2, torch.zeros(4, 4096, dtype=torch.float64)).float()
+    h = f64(T.tern_mx_gate(torch.cat([g, u], dim=1).cuda()))
+    want = O.gate(f64(g), f64(u))
+    off = np.abs(h - want) / np.abs(want)
+    assert off.max() <= 6 * UNIT + 2.0 ** -24, f"{off.max() / UNIT} units"
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lo,hi", [(-83.5, -82.8), (-120, -82), (-190, -110)])
+def test_a_large_factor_brings_a_deep_gate_back(dtype, lo, hi):
+    # u near exp(-g), as far as there are such floats: h is a normal number on both sides of where exp(g) is none
+    g = spread(3, lo, hi).to(dtype)
+    u = powers(4, (-g.double() / np.log(2)).clamp(max=126)).to(dtype)
+    h = f64(T.tern_mx_gate(torch.cat([g, u], dim=1).cuda()))
+    want = O.gate(f64(g), f64(u))
+    assert (np.abs(want) > 2.0 ** -126).mean() > 0.3
+    rel = HALF_ULP[dtype][0]
+    assert (np.abs(h - want) <= np.abs(want) * (6 * UNIT + rel) + LEAST[dtype]).all()
+
+
+def test_ends():
+    inf, nan = float("inf"), float("nan")
+    g = torch.tensor([[0.0, -0.0, 1e30, -1e30, inf, -1e-40, 1e-40, 3e38, -3e38, nan, 0.0, -5.0]])
+    u = torch.tensor([[3e38, 3e38, 1e-30, 3e38, 1.0, 1e30, 1e30, 1.0, 3e38, 1.0, nan, inf]])
+    h = T.tern_mx_gate(torch.cat([g, u], dim=1).cuda()).cpu()[0]
+    assert h[0] == 0 and h[1] == 0 and h[3] == 0 and h[8] == 0
+    assert torch.isposinf(h[4]) and h[7] == g[0, 7] and abs(h[2] - 1) < 1e-6
+    assert abs(h[5] + 5e-11) < 1e-14 and abs(h[6] - 5e-11) < 1e-14
+    assert torch.isnan(h[9]) and torch.isnan(h[10]) and torch.isneginf(h[11])
