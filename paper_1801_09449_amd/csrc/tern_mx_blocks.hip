@@ -123,12 +123,21 @@ __device__ __forceinline__ Decay decay(float g)
     d.r = __builtin_amdgcn_rcpf(1.0f + __builtin_ldexpf(d.m, d.n));
     return d;
 }
-// v e p, |v p| less than 2^9 |v| or a result that overflows too: part of 2^n before the product, which keeps it within a float's range,
-// and the rest behind it.
-__device__ __forceinline__ float decayed(const Decay& d, float v, float p)
+// v e p q, |p| less than 2^9: part of 2^n on v and the rest behind the products, so that none of them leaves a float's range where
+// the result does not (for |v q| up to 2^150).
+__device__ __forceinline__ float decayed(const Decay& d, float v, float p, float q = 1.0f)
 {
     const int first = max(d.n, -32);
-    return __builtin_ldexpf(p * (__builtin_ldexpf(v, first) * d.m), d.n - first);
+    return __builtin_ldexpf(p * (__builtin_ldexpf(v, first) * d.m) * q, d.n - first);
+}
+// Down to here e is a factor like any other.
+constexpr float kDeep = -40.0f;
+__device__ __forceinline__ float least(const float (&v)[8])
+{
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = fminf(m, v[i]);
+    return m;
 }
 
 template <typename T, bool SAVE>
@@ -175,13 +184,30 @@ __global__ __launch_bounds__(kThreads) void gate_grad_kernel(const T* dh, int64_
     load_eight(d, dh + row * ldh + at, n);
     i8_values(g, *reinterpret_cast<const mx_u32x2*>(codes + e * 8), scales[e >> 2]);
     i8_values(u, *reinterpret_cast<const mx_u32x2*>(codes + half * 8), scales[half >> 2]);
+    if (least(g) < kDeep) {             // (few chunks hold any: 2 % of the time if all went this way)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const Decay k = decay(g[i]);
-        const float small = __builtin_ldexpf(k.m, k.n) * k.r, s = g[i] < 0.0f ? small : k.r, less = g[i] < 0.0f ? k.r : small, a = g[i] * s;
-        y[i] = a * u[i];
-        g[i] = d[i] * u[i] * (s + a * less);
-        u[i] = d[i] * a;
+        for (int i = 0; i < 8; ++i) {
+            const Decay k = decay(g[i]);
+            const float a = g[i] * k.r;
+            if (g[i] < 0.0f) {          // s = e r and 1 - s = r: e last, s by itself may have no bits left
+                y[i] = decayed(k, u[i], a);
+                g[i] = decayed(k, u[i], k.r * (1.0f + a), d[i]);
+                u[i] = decayed(k, d[i], a);
+            } else {
+                y[i] = a * u[i];
+                g[i] = d[i] * u[i] * (k.r + a * (__builtin_ldexpf(k.m, k.n) * k.r));
+                u[i] = d[i] * a;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Decay k = decay(g[i]);
+            const float small = __builtin_ldexpf(k.m, k.n) * k.r, s = g[i] < 0.0f ? small : k.r, less = g[i] < 0.0f ? k.r : small, a = g[i] * s;
+            y[i] = a * u[i];
+            g[i] = d[i] * u[i] * (s + a * less);
+            u[i] = d[i] * a;
+        }
     }
     store_eight(dgu + row * ld + at, g, n);
     store_eight(dgu + row * ld + c + at, u, n);

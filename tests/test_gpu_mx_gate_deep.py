@@ -1,9 +1,9 @@
-"""The gate where exp(-|g|) is far below one, in float and bf16, against the 64-bit oracle: as near there as
+"""The gate and its gradient where exp(-|g|) is far below one, in float and bf16, against the 64-bit oracle: as near there as
 at zero.
 
 Bounds in units of 2^-23.  e = exp(-|g|) is 2^n exp2(f), f in (-1, 0] of two fused operations (0.35), exp2 right to its last
-bit (1); 1 / (1 + e): 0.7 of e, 0.5 of the sum, 1 of the reciprocal, 2.2.  h: e, the reciprocal and three products, 5.05,
-taken as 6."""
+bit (1); 1 / (1 + e): 0.7 of e, 0.5 of the sum, 1 of the reciprocal, 2.2.  h and du: e, the reciprocal and three products, 5.05,
+taken as 6.  dg = dh u s (1 + g (1 - s)): its factors' terms round by themselves, 8.75 of |dh u| s (1 + |g|), taken as 10."""
 import numpy as np
 import pytest
 import torch
@@ -50,6 +50,33 @@ def test_a_large_factor_brings_a_deep_gate_back(dtype, lo, hi):
     assert (np.abs(want) > 2.0 ** -126).mean() > 0.3
     rel = HALF_ULP[dtype][0]
     assert (np.abs(h - want) <= np.abs(want) * (6 * UNIT + rel) + LEAST[dtype]).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("large", ["u", "dh", "both"])
+@pytest.mark.parametrize("lo,hi", [(-40, 40), (-83.5, -82.8), (-120, -82), (-160, -110)])
+def test_gradients_of_a_deep_gate(dtype, large, lo, hi):
+    g = spread(5, lo, hi)
+    need = (g.abs() / np.log(2)).clamp(max=126) if hi < 0 else torch.zeros_like(g)
+    share = {"u": 1.0, "dh": 0.0, "both": 0.5}[large]
+    # (a block's u share a scale: one size to a row)
+    u = powers(6, (need.mean(dim=1, keepdim=True) * share).expand_as(g))
+    d = powers(7, need * (1 - share)).to(dtype)
+    _, saved = T.tern_mx_gate(torch.cat([g, u], dim=1).float().cuda(), save=True)
+    v = f64(T.tern_mx_values(saved))
+    dgu, hidden = T.tern_mx_gate_grad(d.cuda(), saved, hidden=True)
+    dg, du = O.gate_grad(f64(d), v[0], v[1])
+    rel, s = HALF_ULP[dtype][0], O.sigmoid(v[0])
+    got = f64(dgu)
+    c = g.shape[1]
+    assert (np.abs(dg) > 2.0 ** -126).mean() > 0.3
+    bound = np.abs(f64(d) * v[1]) * s * (1 + np.abs(v[0])) * 10 * UNIT + rel * np.abs(dg) + LEAST[dtype]
+    assert (np.abs(got[:, :c] - dg) <= bound).all()
+    assert (np.abs(got[:, c:] - du) <= np.abs(du) * (6 * UNIT + rel) + LEAST[dtype]).all()
+    # the hidden values: a step of 1/64 of their block's scale at most from the formula
+    h = O.gate(v[0], v[1])
+    most = np.abs(h).reshape(4, -1, 32).max(axis=2).repeat(32, axis=1)
+    assert (np.abs(f64(T.tern_mx_values(hidden)) - h) <= most / 64 * (1 + 2.0 ** -10) + 2.0 ** -126).all()
 
 
 def test_ends():
