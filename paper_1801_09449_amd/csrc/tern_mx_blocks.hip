@@ -151,11 +151,19 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(const T* gu, int64_t row
     float g[8], u[8], y[8];
     load_eight(g, gu + row * ld + at, n);
     load_eight(u, gu + row * ld + c + at, n);
+    if (least(g) < kDeep) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const Decay d = decay(g[i]);
-        const float a = g[i] * d.r;
-        y[i] = g[i] < 0.0f ? decayed(d, u[i], a) : a * u[i];
+        for (int i = 0; i < 8; ++i) {
+            const Decay d = decay(g[i]);
+            const float a = g[i] * d.r;
+            y[i] = g[i] < 0.0f ? decayed(d, u[i], a) : a * u[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Decay d = decay(g[i]);
+            y[i] = g[i] * d.r * (u[i] * (g[i] < 0.0f ? __builtin_ldexpf(d.m, d.n) : 1.0f));
+        }
     }
     store_eight(h + row * ldh + at, y, n);
     if constexpr (SAVE) {
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(kThreads) void gate_grad_kernel(const T* dh, int64_
     load_eight(d, dh + row * ldh + at, n);
     i8_values(g, *reinterpret_cast<const mx_u32x2*>(codes + e * 8), scales[e >> 2]);
     i8_values(u, *reinterpret_cast<const mx_u32x2*>(codes + half * 8), scales[half >> 2]);
-    if (least(g) < kDeep) {             // (few chunks hold any: 2 % of the time if all went this way)
+    if (least(g) < kDeep) {             // (few chunks hold any; if all went this way: 2 % of the time, and 1 % of the gate's)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const Decay k = decay(g[i]);
