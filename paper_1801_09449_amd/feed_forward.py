@@ -5,6 +5,7 @@ The float weights are the caller's (as the paper keeps full-precision weights be
 before each forward pass); pack() turns them into 4 bits, once for serving and after every optimiser
 step in training.  What a training step keeps for its backward pass is x and both halves of the hidden layer in 8 bits:
 33/32 bytes a value, where a float16 or bfloat16 layer keeps two for each of them and for the product of the halves.
+Gradients are of first order: a backward pass with create_graph=True is an error.
 """
 from typing import Optional
 
@@ -24,6 +25,9 @@ class _Step(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
+        # (a decorator that lets only a derivative of the results fail stays silent where dy is a constant)
+        if torch.is_grad_enabled():
+            raise RuntimeError("the block's gradients cannot be differentiated again (create_graph=True)")
         up, down, x8, halves = ctx.kept
         need_x, need_up, need_down, need_b_up, need_b_down = ctx.needs_input_grad[:5]
         dy = dy.contiguous()
