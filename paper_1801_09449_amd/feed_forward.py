@@ -5,11 +5,13 @@ The float weights are the caller's (as the paper keeps full-precision weights be
 before each forward pass); pack() turns them into 4 bits, once for serving and after every optimiser
 step in training.  What a training step keeps for its backward pass is x and both halves of the hidden layer in 8 bits:
 33/32 bytes a value, where a float16 or bfloat16 layer keeps two for each of them and for the product of the halves.
-Gradients are of first order: a backward pass with create_graph=True is an error.
+Gradients are of first order and of backward mode: a backward pass with create_graph=True is an error, and so is a call on
+tensors with forward-mode tangents.
 """
 from typing import Optional
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from . import binding as B
 
@@ -66,6 +68,10 @@ class FeedForward:
         """x [..., d] (float32, bfloat16 or float16; one token or many) -> [..., d].  Keeps what a backward pass needs
         where one may follow."""
         given = (x, self.w_up, self.w_down, self.b_up, self.b_down)
+        # (a level is asked for first: five tensors took 2 us of a call)
+        if getattr(forward_ad, "_current_level", 0) >= 0 and any(
+                t is not None and forward_ad.unpack_dual(t).tangent is not None for t in given):
+            raise NotImplementedError("the block has no forward-mode derivative")
         if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given):
             return _Step.apply(*given, self.up, self.down)
         return B.tern_mx_linear(B.tern_mx_gate(B.tern_mx_linear(x, self.up, self.b_up)), self.down, self.b_down)

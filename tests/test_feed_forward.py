@@ -2,6 +2,7 @@
 what it hands out, what it refuses to derive, and what it keeps for how long."""
 import pytest
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from paper_1801_09449_amd import binding, feed_forward
 from paper_1801_09449_amd.feed_forward import FeedForward
@@ -80,3 +81,22 @@ def test_a_second_derivative_is_refused(floats, weighted):
         dx, = torch.autograd.grad((f(x) * by).sum(), x, create_graph=True)
         torch.autograd.grad(dx.square().sum() + plain(f, x).sum(), x)
     torch.autograd.grad((f(x) * by).sum(), x)
+
+
+@pytest.mark.parametrize("grad", [True, False], ids=["grad", "no_grad"])
+@pytest.mark.parametrize("which", ["x", "w_up", "w_down", "b_up", "b_down"])
+def test_a_forward_mode_derivative_is_refused(floats, which, grad):
+    f = block(grad=False)
+    x = torch.randn(3, 6, dtype=torch.float64)
+    with forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        f(x)
+        t = x if which == "x" else getattr(f, which)
+        dual = forward_ad.make_dual(t, torch.ones_like(t))
+        if which == "x":
+            x = dual
+        else:
+            setattr(f, which, dual)
+        with pytest.raises(NotImplementedError):
+            f(x)
+    with pytest.raises(NotImplementedError):
+        torch.func.jvp(block(grad=False), (torch.zeros(3, 6, dtype=torch.float64),), (torch.ones(3, 6, dtype=torch.float64),))
