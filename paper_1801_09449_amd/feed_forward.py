@@ -21,7 +21,9 @@ class _Step(torch.autograd.Function):
     def forward(ctx, x, w_up, w_down, b_up, b_down, up, down):
         gu, x8 = B.tern_mx_linear(x, up, b_up, save=True)
         h, halves = B.tern_mx_gate(gu, save=True)
-        ctx.kept = (up, down, x8, halves)            # of this forward pass, whatever is packed later
+        kept = (up, down, x8, halves)                # of this forward pass, whatever is packed later
+        ctx.save_for_backward(*(q.data for q in kept))          # (autograd lets go of them with the backward pass)
+        ctx.blocks = [(q.kind, q.shape) for q in kept]
         ctx.types = [None if t is None else t.dtype for t in (w_up, w_down, b_up, b_down)]
         return B.tern_mx_linear(h, down, b_down)
 
@@ -30,7 +32,7 @@ class _Step(torch.autograd.Function):
         # (a decorator that lets only a derivative of the results fail stays silent where dy is a constant)
         if torch.is_grad_enabled():
             raise RuntimeError("the block's gradients cannot be differentiated again (create_graph=True)")
-        up, down, x8, halves = ctx.kept
+        up, down, x8, halves = (B.MxTensor(t, *of) for t, of in zip(ctx.saved_tensors, ctx.blocks))
         need_x, need_up, need_down, need_b_up, need_b_down = ctx.needs_input_grad[:5]
         dy = dy.contiguous()
         dx = dw_up = dw_down = db_up = db_down = None

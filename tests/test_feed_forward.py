@@ -1,5 +1,8 @@
 """The gated block's autograd on the CPU, with float stand-ins for the library's calls (blocks hold the values themselves):
 what it hands out, what it refuses to derive, and what it keeps for how long."""
+import gc
+import weakref
+
 import pytest
 import torch
 import torch.autograd.forward_ad as forward_ad
@@ -100,3 +103,50 @@ def test_a_forward_mode_derivative_is_refused(floats, which, grad):
             f(x)
     with pytest.raises(NotImplementedError):
         torch.func.jvp(block(grad=False), (torch.zeros(3, 6, dtype=torch.float64),), (torch.ones(3, 6, dtype=torch.float64),))
+
+
+def kept_by(floats, monkeypatch):
+    """Weak references to the checkpoints that forward passes make from here on."""
+    left = []
+
+    def noting(call):
+        def noted(*a, **k):
+            out = call(*a, **k)
+            if k.get("save"):
+                left.append(weakref.ref(out[1].data))
+            return out
+        return noted
+    for name in ("tern_mx_linear", "tern_mx_gate"):
+        monkeypatch.setattr(feed_forward.B, name, noting(getattr(floats, name)))
+    return left
+
+
+def test_the_checkpoint_goes_with_its_backward_pass(floats, monkeypatch):
+    left = kept_by(floats, monkeypatch)
+    f = block()
+    loss = f(torch.randn(3, 6, dtype=torch.float64)).sum()
+    gc.collect()
+    assert len(left) == 2 and all(r() is not None for r in left)
+    loss.backward()
+    gc.collect()
+    assert all(r() is None for r in left)       # though the loss, and its graph, are still there
+    with pytest.raises(RuntimeError):
+        loss.backward()                         # as every other layer says a second time
+    loss = f(torch.randn(3, 6, dtype=torch.float64)).sum()
+    f.w_up.grad = None
+    loss.backward(retain_graph=True)
+    once, f.w_up.grad = f.w_up.grad, None
+    loss.backward()
+    assert torch.equal(f.w_up.grad, once)
+
+
+def test_hooks_on_what_is_saved_see_the_checkpoint(floats):
+    f = block()
+    x = torch.randn(3, 6, dtype=torch.float64)
+    want = torch.autograd.grad(f(x).sum(), f.w_up)[0]
+    packed = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: packed.append(t.clone()) or len(packed) - 1, lambda i: packed[i]):
+        y = f(x)
+    shapes = [tuple(t.shape) for t in packed]
+    assert (3, 6) in shapes and (2, 3, 5) in shapes
+    assert torch.equal(torch.autograd.grad(y.sum(), f.w_up)[0], want)
