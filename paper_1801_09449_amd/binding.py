@@ -922,6 +922,8 @@ def tern_fold_avgpool(w, pool):
 
 
 # ---- block-scaled numbers ------------------------------------------------------------------------
+# Like every call of this module these know nothing of autograd: their results never require a gradient and carry no tangent,
+# whatever their inputs do.  feed_forward.py has the autograd form.
 MX_KINDS = {"f4": 0, "i8": 1}
 FLOAT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
@@ -1020,7 +1022,8 @@ def _workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor)
 
 
 def tern_mx_quantize(x: torch.Tensor, kind: str = "f4") -> MxTensor:
-    """Values (float32, bfloat16 or float16, rows along the last axis) to blocks of 32 with one power of two each."""
+    """Values (float32, bfloat16 or float16, rows along the last axis) to blocks of 32 with one power of two each.  The result is
+    no part of autograd's graph."""
     done = _plain("mx_quantize", "tern_mx_quantize", x, MX_KINDS[kind])
     if done is not None:
         return MxTensor(done, kind, x.shape)
@@ -1031,7 +1034,7 @@ def tern_mx_quantize(x: torch.Tensor, kind: str = "f4") -> MxTensor:
 
 
 def tern_mx_values(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """The values that blocks stand for, exactly (in float16: rounded once)."""
+    """The values that blocks stand for, exactly (in float16: rounded once); no part of autograd's graph."""
     if not isinstance(q, MxTensor):
         raise TypeError("q must be an MxTensor")
     if dtype not in FLOAT_TYPES:
@@ -1058,7 +1061,7 @@ def tern_mx_linear(x: torch.Tensor, w: MxTensor, bias: Optional[torch.Tensor] = 
                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """y = f4(x) w^T + bias on the 4-bit matrix instructions: x [..., c_in], w an "f4" MxTensor [c_out, c_in],
     bias float32 [c_out], y [..., c_out] of x's type.  save=True: returns (y, x as an "i8" MxTensor) for
-    tern_mx_linear_grad."""
+    tern_mx_linear_grad.  y is no part of autograd's graph: its gradients are that call's, or FeedForward's."""
     if w.__class__ is MxTensor and w.kind == "f4" and len(w.shape) == 2:
         done = _plain("mx_linear", "tern_mx_linear", x, w.data, w.shape[0], w.shape[1], bias, bool(save), out, workspace)
         if done is not None:
@@ -1096,7 +1099,8 @@ def tern_mx_linear_grad_workspace_bytes(dtype: torch.dtype, rows: int, c_in: int
 def tern_mx_linear_grad(dy: torch.Tensor, w: Optional[MxTensor], saved: Optional[MxTensor], bias: bool = False,
                         workspace: Optional[torch.Tensor] = None):
     """Gradients of tern_mx_linear, straight through its roundings: (dx, dw, db) with dx = dy w in dy's type,
-    dw = dy^T saved and db = the sums of dy's columns (bias=True) in float32.  w None: no dx; saved None: no dw."""
+    dw = dy^T saved and db = the sums of dy's columns (bias=True) in float32.  w None: no dx; saved None: no dw.  No
+    part of autograd's graph: there is no second derivative."""
     good = all(q is None or q.__class__ is MxTensor for q in (w, saved)) and not (w is None and saved is None and not bias)
     if good and (w is None or w.kind == "f4" and len(w.shape) == 2) and (saved is None or saved.kind == "i8"):
         # (the compiled path sees bytes and c_in: other extents may fill up to as many bytes)
@@ -1131,7 +1135,7 @@ def tern_mx_linear_grad(dy: torch.Tensor, w: Optional[MxTensor], saved: Optional
 
 def tern_mx_gate(gu: torch.Tensor, save: bool = False, out: Optional[torch.Tensor] = None):
     """h = silu(g) u with g and u the halves of gu's last axis.  save=True: returns (h, (g, u) as one "i8" MxTensor of
-    shape [2, ..., c]) for tern_mx_gate_grad."""
+    shape [2, ..., c]) for tern_mx_gate_grad.  h is no part of autograd's graph: its gradient is that call's, or FeedForward's."""
     done = _plain("mx_gate", "tern_mx_gate", gu, bool(save), out)
     if done is not None:
         return (done[0], MxTensor(done[1], "i8", (2, *gu.shape[:-1], gu.shape[-1] // 2))) if save else done
@@ -1149,7 +1153,8 @@ def tern_mx_gate(gu: torch.Tensor, save: bool = False, out: Optional[torch.Tenso
 
 def tern_mx_gate_grad(dh: torch.Tensor, saved: MxTensor, hidden: bool = False, out: Optional[torch.Tensor] = None):
     """Gradient of tern_mx_gate at the values that it saved: dgu [..., 2 c] for dh [..., c].  hidden=True: returns
-    (dgu, h of the saved values as an "i8" MxTensor), the saved input of the layer that follows the gate."""
+    (dgu, h of the saved values as an "i8" MxTensor), the saved input of the layer that follows the gate.  No part of
+    autograd's graph: there is no second derivative."""
     if saved.__class__ is MxTensor and saved.kind == "i8" and saved.shape[1:] == tuple(dh.shape):
         done = _plain("mx_gate_grad", "tern_mx_gate_grad", dh, saved.data, bool(hidden), out)
         if done is not None:
