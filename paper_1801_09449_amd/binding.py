@@ -924,8 +924,19 @@ def tern_fold_avgpool(w, pool):
 # ---- block-scaled numbers ------------------------------------------------------------------------
 # Like every call of this module these know nothing of autograd: their results never require a gradient and carry no tangent,
 # whatever their inputs do.  feed_forward.py has the autograd form.
-MX_KINDS = {"f4": 0, "i8": 1}
-FLOAT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+class _Names(dict):
+    """What is not there is refused by name."""
+
+    def __init__(self, of, error, what):
+        super().__init__(of)
+        self.error, self.what = error, what
+
+    def __missing__(self, key):
+        raise self.error(f"{self.what}, got {key!r}")
+
+
+MX_KINDS = _Names({"f4": 0, "i8": 1}, KeyError, "kind must be 'f4' or 'i8'")
+FLOAT_TYPES = _Names({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}, TypeError, "dtype must be float32, bfloat16 or float16")
 
 
 class MxTensor:
@@ -1037,10 +1048,9 @@ def tern_mx_values(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optiona
     """The values that blocks stand for, exactly (in float16: rounded once); no part of autograd's graph."""
     if not isinstance(q, MxTensor):
         raise TypeError("q must be an MxTensor")
-    if dtype not in FLOAT_TYPES:
-        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    kind, t = MX_KINDS[q.kind], FLOAT_TYPES[dtype]
     if out is None:
-        done = _plain("mx_values", "tern_mx_values", q.data, MX_KINDS[q.kind], q.shape, FLOAT_TYPES[dtype])
+        done = _plain("mx_values", "tern_mx_values", q.data, kind, q.shape, t)
         if done is not None:
             return done
         out = torch.empty(q.shape, dtype=dtype, device=q.data.device)
@@ -1048,7 +1058,7 @@ def tern_mx_values(q: MxTensor, dtype: torch.dtype = torch.float32, out: Optiona
         raise ValueError(f"out must have shape {q.shape}")
     t, rows, cols, ld = _matrix(out, "out", dtype)
     _same_device(q.data, out=out)
-    _check(lib().tern_mx_values(_blocks(q, q.kind, rows, cols, "q"), MX_KINDS[q.kind], rows, cols, t, _ptr(out), ld,
+    _check(lib().tern_mx_values(_blocks(q, q.kind, rows, cols, "q"), kind, rows, cols, t, _ptr(out), ld,
                                 _stream(out)), "tern_mx_values")
     return out
 
@@ -1105,7 +1115,7 @@ def tern_mx_linear_grad(dy: torch.Tensor, w: Optional[MxTensor], saved: Optional
     if good and (w is None or w.kind == "f4" and len(w.shape) == 2) and (saved is None or saved.kind == "i8"):
         # (the compiled path sees bytes and c_in: other extents may fill up to as many bytes)
         c_in = w.cols if w is not None else saved.cols if saved is not None else 1
-        if dy.__class__ is torch.Tensor and dy.dim() > 0 and (w is None or w.shape[0] == dy.shape[-1]) and (
+        if isinstance(dy, torch.Tensor) and dy.dim() > 0 and (w is None or w.shape[0] == dy.shape[-1]) and (
                 saved is None or saved.shape == (*dy.shape[:-1], c_in)):
             done = _plain("mx_linear_grad", "tern_mx_linear_grad", dy, None if w is None else w.data,
                           None if saved is None else saved.data, c_in, bool(bias), workspace)
@@ -1155,7 +1165,7 @@ def tern_mx_gate_grad(dh: torch.Tensor, saved: MxTensor, hidden: bool = False, o
     """Gradient of tern_mx_gate at the values that it saved: dgu [..., 2 c] for dh [..., c].  hidden=True: returns
     (dgu, h of the saved values as an "i8" MxTensor), the saved input of the layer that follows the gate.  No part of
     autograd's graph: there is no second derivative."""
-    if saved.__class__ is MxTensor and saved.kind == "i8" and saved.shape[1:] == tuple(dh.shape):
+    if saved.__class__ is MxTensor and saved.kind == "i8" and isinstance(dh, torch.Tensor) and saved.shape[1:] == dh.shape:
         done = _plain("mx_gate_grad", "tern_mx_gate_grad", dh, saved.data, bool(hidden), out)
         if done is not None:
             return (done[0], MxTensor(done[1], "i8", dh.shape)) if hidden else done
