@@ -41,17 +41,23 @@ def only(v, at):
 
 
 def places(n, count, turn):
-    """One of n for each of `count`, spread over all of n."""
-    return (torch.arange(count) * max(1, n // count) + 37 * turn) % n
+    """One of n for each of `count`, from the first to the last of n."""
+    if count >= n:
+        return (torch.arange(count) + turn) % n
+    return ((torch.arange(count) * (n - 1)).div(max(1, count - 1), rounding_mode="floor") + turn) % n
+
+
+def operands(rows, c_in, c_out, dtype, turn):
+    """(dy, w or None, x or None): the three ways in which sums are exact."""
+    dy, w, x = full(turn, rows, c_out, dtype), some(10 + turn, c_out, c_in), some(20 + turn, rows, c_in)
+    return ((dy, only(w, places(c_out, c_in, turn)), only(x, places(rows, c_in, turn))),
+            (only(dy.t().contiguous(), places(c_out, rows, turn)).t().contiguous(), w, None),
+            (only(dy, places(rows, c_out, turn)), None, x))
 
 
 def check(rows, c_in, c_out, dtype):
     for turn in range(3):
-        dy, w, x = full(turn, rows, c_out, dtype), some(10 + turn, c_out, c_in), some(20 + turn, rows, c_in)
-        cases = ((dy, only(w, places(c_out, c_in, turn)), only(x, places(rows, c_in, turn))),
-                 (only(dy.t().contiguous(), places(c_out, rows, turn)).t().contiguous(), w, None),
-                 (only(dy, places(rows, c_out, turn)), None, x))
-        for d, a, b in cases:
+        for d, a, b in operands(rows, c_in, c_out, dtype, turn):
             q = None if a is None else T.tern_mx_quantize(a.cuda(), "f4")
             s = None if b is None else T.tern_mx_quantize(b.cuda(), "i8")
             dx, dw, _ = T.tern_mx_linear_grad(d.cuda(), q, s)
@@ -71,12 +77,15 @@ def forced(form, splits):
     T.tern_set_option(SPLITS, splits)
 
 
+FORMS = [(40, 33, 300), (300, 270, 130), (513, 140, 700), (129, 513, 1030)]
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("form,splits", [(f, s) for f in (1, 2, 3, 4) for s in (1, 3)])
 def test_every_form_has_all_bits(form, splits, dtype):
     forced(form, splits)
     try:
-        for size in ((40, 33, 300), (300, 270, 130), (513, 140, 700), (129, 513, 1030)):
+        for size in FORMS:
             check(*size, dtype)
     finally:
         forced(0, 0)
@@ -99,7 +108,10 @@ def test_narrow_layers_have_all_bits(splits, dtype):
         forced(0, 0)
 
 
+CHOSEN = [(4100, 40, 4099), (16, 4096, 4100), (4099, 4100, 24), (4100, 100, 8300), (600, 700, 800)]
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
-@pytest.mark.parametrize("size", [(4100, 40, 4099), (16, 4096, 4100), (4099, 4100, 24), (4100, 100, 8300), (600, 700, 800)])
+@pytest.mark.parametrize("size", CHOSEN)
 def test_what_is_chosen_has_all_bits(size, dtype):
     check(*size, dtype)
