@@ -3,8 +3,8 @@
 //
 // A lane takes eight neighbouring values, a block of 32 is four lanes of a quad, and the block's largest magnitude
 // crosses them by two lane permutations.  Measured: 16384 x 4096 bf16 to 4 bits 34 us (5.0 TB/s) and back 26 (6.6); the gate of
-// 8192 x 8192 bf16 with its halves saved 87 to 102 us (5.3 to 6.2), the gradient at 8001 x 8190 (rows at any multiple of
-// four bytes) 121 to 127 (4.8).
+// 8192 x 8192 bf16 with its halves saved 90 to 101 us (5.4 to 6.0), the gradient at 8001 x 8190 (rows at any multiple of
+// four bytes) 121 to 128 (4.7 to 4.9).
 #include "tern_mx_common.h"
 #include "tern_division.h"
 

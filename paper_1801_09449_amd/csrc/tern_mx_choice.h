@@ -40,8 +40,8 @@ inline int64_t tiles_of(int form, const ProductSize& s)
 // with and without the other.)  The time that is made least, in microseconds:
 //   a workgroup's steps of a record each (direct: every wave's own) and what it takes to set up and to leave;
 //   256 compute units work at once, in turns where there are more workgroups;
-//   all of them together take in 16 MB a microsecond (a tile of 256 x 256 takes 0.66 us for a step's 68 KB with half of
-//   the compute units at work and 1.3 with all);
+//   all of them together take in 16 MB a microsecond at best (a step's 68 KB of a 256 x 256 tile, fetched and not multiplied:
+//   0.66 us with half of the compute units at work, 1.3 with all; multiplied, 1.05 and 1.2 to 1.5);
 //   sums of splits go through memory twice, in a launch of their own.
 // forced_form, forced_splits: -1 and 0, or what a tuning override asks for.
 inline void product_plan(bool f4, const ProductSize* s, int n, int forced_form, int forced_splits, ProductPlan* best)

@@ -51,9 +51,10 @@ __device__ __forceinline__ void arrive()
 // Which product, tile and share of k a workgroup has; false: none.  Workgroups go to the eight XCDs in turn: each takes a
 // run of tiles, in bands of so many tiles of B by all of A, so that what neighbours read meets in its L2, and of one share of k
 // before the next (against a run of every share's: gradients of 512 x 1024 -> 4096 in float 43.9 us for 47.5, of 23 x 1365 ->
-// 3688 in half precision 25.6 for 30.3).  8192 x 4096 -> 16384 in 4 bits with bands of 2, 3, 5 and 6: 310 us, 4: 320, 8 and
-// 16: 334; the gradients of a layer of 8192 x 4096 -> 8192 with any of them up to 8: 891 to 907, 16: 912.  (Bands that are
-// square in bytes, so narrower for a B in parts: between 5 % faster and 8 % slower.)
+// 3688 in half precision 25.6 for 30.3).  8192 x 4096 -> 16384 in 4 bits: bands of 2, 3, 5 and 6 are
+// alike, one of 4 takes 3 % longer, of 8 or 16 8 %; the gradients of a layer of 8192 x 4096 -> 8192 are alike to 2 % with any of
+// them up to 8 and take 2 % more with 16.  (Bands that are square in bytes, so narrower for a B in parts:
+// between 5 % faster and 8 % slower.)
 constexpr int kBand = 6;
 struct Place {
     int tile_a, tile_b, split;
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(WA * WB * 64, UA * UB * PARTS > 4 ? 1 : 2) void til
 
     // Results leave by way of LDS, a region for each wave: 32 rows of B at a time, so that a store covers whole lines.
     // PAST: past the caches, for outputs that would not stay there anyhow (of 128 MB or more): their lines are then not in
-    // the way of what comes next.  8192 x 4096 -> 16384 in bf16 (268 MB) 294 -> 284 us.
+    // the way of what comes next.  8192 x 4096 -> 16384 in bf16 (268 MB out), all of the call, 294 -> 284 us.
     auto leave = [&](auto* to, int64_t ld, auto past) {
         typedef std::remove_pointer_t<decltype(to)> T;
         constexpr int kVec = 16 / (int)sizeof(T), kRowLanes = 32 * UA / kVec, kRows = 64 / kRowLanes;
